@@ -423,9 +423,11 @@ nld_status_t nld_kv_commit(const nld_attn_params_t *params, const void *k_new, c
  * the rows cu_tokens[b] .. cu_tokens[b + 1] - 1 (0 = cu_tokens[0] <= ... <=
  * cu_tokens[B] = T; a sequence may have none). With cu_tokens NULL every
  * sequence has T / B rows (T a multiple of B). Row j of sequence b is logical
- * slot lens[b] + j, wherever its page lies. Rows that cu_tokens does not
- * cover, slots past the page table and page ids outside the pool are flagged
- * in nld_device_error and nothing is written for them.
+ * slot lens[b] + j, wherever its page lies. Slots past the page table and page
+ * ids outside the pool are flagged in nld_device_error and nothing is written
+ * for them (the read-back writes 0). A cu_tokens that does not ascend from 0 to
+ * T is flagged too (NLD_DEVERR_PREFIX_RANGE), and nothing is written for rows
+ * that it gives to no sequence.
  *
  * Rotation. Channel pairs of the first rotary_dim channels of each query and
  * key head turn by the angle of their row's position (positions[r], or the
@@ -524,7 +526,8 @@ nld_status_t nld_rope_append_kv4(const nld_attn_params_t *params, const nld_appe
 /*
  * Read T rows of a 4-bit cache back as the bf16 values they stand for: row j
  * of sequence b is logical slot starts[b] + j (starts NULL: from slot 0).
- * Rows whose slot or page is out of range read as 0 and are flagged.
+ * Rows whose slot or page is out of range read as 0 and are flagged; rows that
+ * cu_tokens gives to no sequence are left as they are (flagged as above).
  *   k_out, v_out bf16 [T, Hkv, D], 16-byte aligned
  */
 nld_status_t nld_kv4_read(const nld_attn_params_t *params, const void *kv4_pages,

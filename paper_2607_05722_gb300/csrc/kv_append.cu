@@ -90,6 +90,18 @@ __device__ __forceinline__ void write_lens(const AppendArgs& a, int first, int s
     a.new_lens[b] = a.lens[b] + static_cast<int>(max(row_begin(a, b + 1) - row_begin(a, b), 0l));
 }
 
+// The rows belong to sequences only as cu_tokens says: it has to ascend from 0
+// to T. Its entries are dealt to the grid's threads, after their rows' work, so
+// that nothing waits for these loads.
+__device__ __forceinline__ void check_cover(const AppendArgs& a) {
+  if (a.cu == nullptr) return;
+  const long threads = static_cast<long>(gridDim.x) * kRowThreads;
+  for (long i = static_cast<long>(blockIdx.x) * kRowThreads + threadIdx.x; i <= a.B; i += threads) {
+    const int at = __ldg(a.cu + i), before = i > 0 ? __ldg(a.cu + i - 1) : 0;
+    if (at < before || (i == 0 && at != 0) || (i == a.B && at != a.T)) atomicOr(a.err, NLD_DEVERR_PREFIX_RANGE);
+  }
+}
+
 // `threads` threads (a warp or a CTA; tid is the one's number) rotate or copy
 // the heads of packed row r: the queries (when present), then K, then V.
 template <bool kWithKv>
@@ -184,6 +196,7 @@ __global__ void __launch_bounds__(kRowThreads) rope_append_kernel(AppendArgs a, 
   grid_dependency_wait();  // the rows, lengths and tables come from earlier kernels
   if (a.fuse_lens && blockIdx.x == 0) write_lens(a, threadIdx.x, kRowThreads);
   append_rows<true>(a, blockIdx.x, by_warp);
+  check_cover(a);
 }
 
 __global__ void __launch_bounds__(kRowThreads) advance_lens_kernel(AppendArgs a) {
@@ -453,6 +466,7 @@ __global__ void __launch_bounds__(kRowThreads, 9) rope_append_kv4_kernel(AppendA
   } else {
     append_rows<false>(a, blockIdx.x - min(before, units * 2 * parts), by_warp);
   }
+  check_cover(a);
 }
 
 // Values of a word in storage order with one (a, c) pair for all.
@@ -470,10 +484,7 @@ __device__ __forceinline__ uint4 word_values(uint32_t w, uint32_t scale) {
 // are 16 bytes apart beyond their length, so that the 8 tokens of a store lie
 // in different banks. With 12 CTAs to an SM: 34 us, 5.2 TB/s.
 template <int D>
-__global__ void __launch_bounds__(kRowThreads, 12) kv4_read_kernel(AppendArgs a, int parts, int per) {
-  extern __shared__ __align__(128) unsigned char rows[];  // [2][16] of per heads
-  grid_launch_dependents();
-  grid_dependency_wait();
+__device__ __forceinline__ void read_unit(const AppendArgs& a, int parts, int per, unsigned char* rows) {
   constexpr int kWays = kGroupWarps / Rec<D>::kGroups;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = warp % Rec<D>::kGroups;
@@ -522,6 +533,15 @@ __global__ void __launch_bounds__(kRowThreads, 12) kv4_read_kernel(AppendArgs a,
     }
     bulk_store_wait_read();
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kRowThreads, 12) kv4_read_kernel(AppendArgs a, int parts, int per) {
+  extern __shared__ __align__(128) unsigned char rows[];  // [2][16] of per heads
+  grid_launch_dependents();
+  grid_dependency_wait();
+  read_unit<D>(a, parts, per, rows);
+  check_cover(a);
 }
 
 // CTAs per unit: the heads are shared out until there are about 8 CTAs to an SM
