@@ -411,7 +411,9 @@ def nld_kv_commit(params: AttnParams, k_new, v_new, counts, page_table, prefix_l
 
 
 def _rows(t: torch.Tensor, shape, name: str) -> int:
-    """Row stride of a CUDA bf16 [T, heads, dim] tensor whose rows hold their heads contiguously."""
+    """Row stride of a CUDA bf16 [T, heads, dim] tensor whose rows hold their heads contiguously.
+    Rows that share storage (a broadcast tensor: stride 0, which the C ABI takes
+    for contiguous) are refused."""
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {torch.bfloat16}")
     if t.shape != shape:
@@ -419,7 +421,12 @@ def _rows(t: torch.Tensor, shape, name: str) -> int:
     row, head, dim = t.stride()
     if not t.is_cuda or dim != 1 or (shape[1] > 1 and head != shape[2]):
         raise ValueError(f"{name}: must be a CUDA tensor with contiguous heads")
-    return row if shape[0] > 1 else shape[1] * shape[2]
+    width = shape[1] * shape[2]
+    if shape[0] <= 1:
+        return width
+    if row < width:
+        raise ValueError(f"{name}: rows overlap (stride {row}, {width} elements each)")
+    return row
 
 
 def _append(entry, params, q, k_new, v_new, rope, page_table, lens, caches, q_out, cu_tokens, positions, style,
