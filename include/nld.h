@@ -561,11 +561,11 @@ nld_status_t nld_block_attn_kv4_masked(const nld_attn_params_t *params, const vo
                                        size_t workspace_bytes, cudaStream_t stream);
 
 /*
- * Failure-detection check: launches one thread that waits, with the same
- * bounded wait every pipeline uses, on an mbarrier nothing ever arrives on.
- * After limit_ns nanoseconds (1 .. 1e9) the wait gives up, sets
- * NLD_DEVERR_WAIT_TIMEOUT in the device error word and the kernel returns;
- * the context stays usable. For tests and diagnostics.
+ * Failure-detection check: launches one warp that waits on an mbarrier nothing
+ * ever arrives on, with each of the bounded waits the pipelines use (three, one
+ * after the other). Each gives up after limit_ns nanoseconds (1 .. 1e9); once
+ * all have, NLD_DEVERR_WAIT_TIMEOUT is set in the device error word and the
+ * kernel returns; the context stays usable. For tests and diagnostics.
  * Errors: NLD_ERR_INVALID_ARG (limit out of range), NLD_ERR_CUDA (launch).
  */
 nld_status_t nld_check_wait_timeout(uint64_t limit_ns, cudaStream_t stream);

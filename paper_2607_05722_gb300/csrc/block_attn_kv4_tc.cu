@@ -126,53 +126,6 @@ __device__ __forceinline__ void set_regs_up() { asm volatile("setmaxnreg.inc.syn
 template <int N>
 __device__ __forceinline__ void set_regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// Waits for an mbarrier phase, all lanes together, for at most 2^24 attempts
-// (about a second: an attempt takes 80 cycles or more); then flags the timeout
-// and returns false. One tight loop without clock or lane tests, because these
-// waits are most of what the issuing warps execute and their code must stay in
-// the instruction cache. kPatient: for warps that run ahead of the others;
-// they sleep between attempts, which otherwise take issue slots from working
-// warps (2^20 attempts then).
-template <bool kPatient = false>
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned int* err) {
-  uint32_t ok;
-  if constexpr (kPatient) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
-        "mov.u32 n, 0;\n\t"
-        "AGAIN_%=:\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "@p bra DONE_%=;\n\t"
-        "nanosleep.u32 100;\n\t"
-        "add.u32 n, n, 1;\n\t"
-        "setp.lt.u32 q, n, 1048576;\n\t"
-        "@q bra AGAIN_%=;\n\t"
-        "DONE_%=:\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
-        "mov.u32 n, 0;\n\t"
-        "AGAIN_%=:\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "@p bra DONE_%=;\n\t"
-        "add.u32 n, n, 1;\n\t"
-        "setp.lt.u32 q, n, 16777216;\n\t"
-        "@q bra AGAIN_%=;\n\t"
-        "DONE_%=:\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-  }
-  if (__all_sync(0xffffffffu, ok != 0)) return true;
-  atomicOr(err, NLD_DEVERR_WAIT_TIMEOUT);
-  return false;
-}
-
 // One lane of a converged warp. The compiler keeps what it guards in uniform
 // registers, where the MMA descriptors have to be: an MMA is issued every 12
 // to 31 cycles (N = 16 to 64), against about 100 behind a test of the lane

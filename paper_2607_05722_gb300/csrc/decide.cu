@@ -140,17 +140,26 @@ cudaError_t launch_unmask_threshold(const float* conf, int B, int n, float thres
                        threshold, pos, nsel);
 }
 
-// One thread initialises an mbarrier that expects one arrival, never
-// arrives, and waits on it with the pipelines' bounded wait: the wait gives
-// up after limit_ns and records NLD_DEVERR_WAIT_TIMEOUT, as any kernel's
-// wait would, and the kernel returns.
+// One warp waits on an mbarrier that nothing arrives on with each of the
+// pipelines' bounded waits in turn: a thread's, a warp's, and a warp's that
+// sleeps between its attempts. Each has to give up after limit_ns and say so;
+// NLD_DEVERR_WAIT_TIMEOUT is recorded once all three have, and the kernel returns.
 __global__ void __launch_bounds__(32) wait_timeout_check_kernel(uint64_t limit_ns, unsigned int* err) {
   __shared__ uint64_t bar;
+  __shared__ unsigned int word[3];
   if (threadIdx.x == 0) {
+    word[0] = word[1] = word[2] = 0;
     mbar_init(&bar, 1);
     fence_mbar_init();
-    mbar_wait_for(&bar, 0, err, limit_ns);
   }
+  __syncwarp();
+  bool gave_up = threadIdx.x != 0 || !mbar_wait_for(&bar, 0, &word[0], limit_ns);
+  __syncwarp();
+  gave_up = !warp_wait_for<false>(&bar, 0, &word[1], limit_ns) && gave_up;
+  gave_up = !warp_wait_for<true>(&bar, 0, &word[2], limit_ns) && gave_up;
+  __syncwarp();
+  gave_up = gave_up && (word[0] & word[1] & word[2] & NLD_DEVERR_WAIT_TIMEOUT) != 0;
+  if (__all_sync(0xffffffffu, gave_up) && threadIdx.x == 0) atomicOr(err, NLD_DEVERR_WAIT_TIMEOUT);
 }
 
 cudaError_t launch_wait_timeout_check(uint64_t limit_ns, unsigned int* err, cudaStream_t stream) {

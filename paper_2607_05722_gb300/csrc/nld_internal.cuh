@@ -58,7 +58,7 @@ struct TmaMaps {
 cudaError_t launch_block_attn_tc(const AttnArgs& a, const TmaMaps& maps, int head_dim, cudaStream_t stream);
 // The same for a table mask (a.mode == kModeBlockMask; block_attn_tc_masked.cu).
 cudaError_t launch_block_attn_tc_masked(const AttnArgs& a, const TmaMaps& maps, int head_dim, cudaStream_t stream);
-// A kernel whose one mbarrier wait can never complete (decide.cu).
+// A kernel whose mbarrier waits can never complete (decide.cu).
 cudaError_t launch_wait_timeout_check(uint64_t limit_ns, unsigned int* err, cudaStream_t stream);
 cudaError_t launch_combine(const __nv_bfloat16* o_part, const float* lse_part, int S, int B, int Hq, int bl,
                            int D, __nv_bfloat16* out, float* lse, int sm_count, cudaStream_t stream);
@@ -211,6 +211,62 @@ __device__ __forceinline__ bool mbar_wait_for(uint64_t* bar, uint32_t parity, un
 }
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsigned int* err) {
   return mbar_wait_for(bar, parity, err, kWaitLimitNs);
+}
+
+// The same by all lanes of a warp together, for kernels whose issuing warps
+// execute little else: one tight loop without lane tests, because its code must
+// stay in the instruction cache. Its clock is the SM's cycle counter, read after
+// every attempt, as an attempt may be suspended for a time that is the
+// hardware's choice: 2.1 cycles are at least a nanosecond (2070 MHz at most), and
+// the limit in them fits the counter's low word. (The timer in nanoseconds costs
+// registers and rounds of attempts: 155 rows, 16 sequences of 8192 to 16384
+// tokens 192 us, this way 186.) kPatient: for warps that run ahead of the others;
+// they sleep between attempts, which otherwise take issue slots from working warps.
+template <bool kPatient>
+__device__ __forceinline__ bool warp_wait_for(uint64_t* bar, uint32_t parity, unsigned int* err, uint64_t limit_ns) {
+  const uint32_t cycles = static_cast<uint32_t>(limit_ns * 21 / 10);
+  uint32_t ok;
+  if constexpr (kPatient) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 t, t0;\n\t"
+        "mov.u32 t0, %%clock;\n\t"
+        "AGAIN_%=:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE_%=;\n\t"
+        "nanosleep.u32 100;\n\t"
+        "mov.u32 t, %%clock;\n\t"
+        "sub.u32 t, t, t0;\n\t"
+        "setp.lt.u32 q, t, %3;\n\t"
+        "@q bra AGAIN_%=;\n\t"
+        "DONE_%=:\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(cycles)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 t, t0;\n\t"
+        "mov.u32 t0, %%clock;\n\t"
+        "AGAIN_%=:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE_%=;\n\t"
+        "mov.u32 t, %%clock;\n\t"
+        "sub.u32 t, t, t0;\n\t"
+        "setp.lt.u32 q, t, %3;\n\t"
+        "@q bra AGAIN_%=;\n\t"
+        "DONE_%=:\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(cycles)
+        : "memory");
+  }
+  if (__all_sync(0xffffffffu, ok != 0)) return true;
+  atomicOr(err, NLD_DEVERR_WAIT_TIMEOUT);
+  return false;
+}
+template <bool kPatient = false>
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned int* err) {
+  return warp_wait_for<kPatient>(bar, parity, err, kWaitLimitNs);
 }
 
 // 4-D tiled TMA load into shared memory, completing on an mbarrier.

@@ -559,8 +559,8 @@ def nld_block_attn_plan(params: AttnParams, block_len: int, sm_count: int) -> di
 
 
 def nld_check_wait_timeout(limit_ns: int, stream=None) -> None:
-    """Launch the bounded-wait check: one wait that nothing completes gives up
-    after limit_ns and sets NLD_DEVERR_WAIT_TIMEOUT."""
+    """Launch the bounded-wait check: each of the pipelines' waits gives up after
+    limit_ns on a barrier that nothing completes; then NLD_DEVERR_WAIT_TIMEOUT is set."""
     _check(lib().nld_check_wait_timeout(ctypes.c_uint64(int(limit_ns)), _stream(stream)),
            "nld_check_wait_timeout")
 
