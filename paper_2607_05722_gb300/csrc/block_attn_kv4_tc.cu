@@ -30,10 +30,11 @@
 // bf16 and fp32, so one reference for all rows of a group will do as long as
 // their terms 2^(score - reference) stay well inside the exponent range. The
 // reference is the largest score of the unit's first token plus 45, so there
-// is room for scores 2^46 times that token's and for rows 2^55 below it. A
+// is room for scores 2^46 times that token's and for rows 2^40 below it. A
 // term of 2 or more sets a bit of its packed bf16 that no smaller one has (one
 // logic operation per three words); a row whose terms are too small shows in
-// its sum. A unit that trips either check writes nothing and is run again at
+// its sum. (Padding rows score 0 and take part in the first check: a group with
+// some is run again where its first token scores below some -46.) A unit that trips either check writes nothing and is run again at
 // the end of the batch, once for its rows' maxima and once with the scores
 // taken relative to them. Row sums stay per lane in fp32 until the end.
 //
@@ -49,7 +50,10 @@ namespace {
 constexpr int kTok = 128;                   // tokens per tile (lanes of A)
 constexpr int kTileRecs = kTok / kRecTok;   // 8
 constexpr float kHead = 45.f;               // log2 room above the score a reference is taken from
-constexpr float kTiny = 0x1p-100f;          // smallest row sum taken at its word
+// Smallest row sum taken at its word. Terms below 2^-126 are lost, and so is a
+// partial 2^126 below another in the merge: of n tokens, n 2^-41 of such a sum
+// (2^-11 at the 2^30 tokens that a page table may hold).
+constexpr float kTiny = 0x1p-85f;
 constexpr int kSoftBar = 1;                 // named barriers: all softmax warps; 2, 3: a group
 constexpr int kBatch = 32;                  // segments handed to the roles at a time
 enum Mode { kFirstToken = 0, kMaxima = 1, kKnownMaxima = 2 };  // where a unit's references come from
