@@ -36,10 +36,6 @@ __device__ __forceinline__ Vec8 unpack8(uint4 w) {
   return r;
 }
 
-__device__ __forceinline__ Vec8 load8(const __nv_bfloat16* p) {
-  return unpack8(*reinterpret_cast<const uint4*>(p));  // may be rotated in place: not the read-only path
-}
-
 __device__ __forceinline__ uint4 pack8(const Vec8& v) {
   return make_uint4(pack_bf16(v.x[0], v.x[1]), pack_bf16(v.x[2], v.x[3]), pack_bf16(v.x[4], v.x[5]),
                     pack_bf16(v.x[6], v.x[7]));
@@ -156,20 +152,26 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, long r, int tid,
       src = turns ? a.k + r * a.k_stride + kh * a.D : a.v + r * a.v_stride + kh * a.D;
       dst = (turns ? a.k_pages : a.v_pages) + cell + static_cast<long>(kh) * a.P * a.D;
     }
-    Vec8 x = load8(src + d0), y = load8(src + d1);
-    if (turns && halves) {
+    // (may be rotated in place: not the read-only path)
+    uint4 w0 = *reinterpret_cast<const uint4*>(src + d0), w1 = *reinterpret_cast<const uint4*>(src + d1);
+    if (turns && (halves || within)) {  // else the bits as they are, a NaN's too
+      Vec8 x = unpack8(w0), y = unpack8(w1);
+      if (halves) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float lo = x.x[e], hi = y.x[e];
-        x.x[e] = turn_lo(lo, hi, c.x[e], s.x[e]);
-        y.x[e] = turn_hi(hi, lo, c.x[e], s.x[e]);
+        for (int e = 0; e < 8; ++e) {
+          const float lo = x.x[e], hi = y.x[e];
+          x.x[e] = turn_lo(lo, hi, c.x[e], s.x[e]);
+          y.x[e] = turn_hi(hi, lo, c.x[e], s.x[e]);
+        }
+      } else {
+        turn_within(x, c.x, s.x);
+        turn_within(y, c.x + 4, s.x + 4);
       }
-    } else if (turns && within) {
-      turn_within(x, c.x, s.x);
-      turn_within(y, c.x + 4, s.x + 4);
+      w0 = pack8(x);
+      w1 = pack8(y);
     }
-    *reinterpret_cast<uint4*>(dst + d0) = pack8(x);
-    *reinterpret_cast<uint4*>(dst + d1) = pack8(y);
+    *reinterpret_cast<uint4*>(dst + d0) = w0;
+    *reinterpret_cast<uint4*>(dst + d1) = w1;
   }
 }
 
