@@ -1,6 +1,7 @@
 // C ABI of libnld (include/nld.h): host-side argument checks, KV split choice,
 // TMA descriptor encoding and kernel launches. Nothing here allocates device
 // memory or synchronises, except nld_device_error().
+#include <cfloat>
 #include <climits>
 #include <math.h>
 #include <stdio.h>
@@ -748,7 +749,8 @@ nld_status_t block_attn_kv4_impl(const nld_attn_params_t* params, const void* q_
     a.part_ml = reinterpret_cast<float2*>(base + w.ml_at);
   }
   const float scale = params->softmax_scale > 0.f ? params->softmax_scale : 1.0f / sqrtf((float)params->head_dim);
-  a.scale_log2 = scale * nld::kLog2e;
+  // the kernels' paired FMAs flush subnormals, and 0 times a hidden cell's -inf is NaN
+  a.scale_log2 = fmaxf(scale * nld::kLog2e, FLT_MIN);
   a.inv_scale_log2 = 1.0f / a.scale_log2;
   a.B = params->batch;
   a.Hq = params->num_q_heads;
