@@ -542,7 +542,9 @@ size_t nld_block_attn_kv4_workspace_size(const nld_attn_params_t *params, int bl
  * nld_block_attn over a 4-bit cache: the same masks, shapes and outputs, with
  * K and V the values the cells stand for. Work is divided evenly over the SMs
  * on the device, from prefix_lens, so params->num_splits must be 0; the flags
- * are accepted.
+ * are accepted and change nothing. Where a sequence is cut depends on the
+ * lengths of all of them, so the last bits of its outputs do too; the same call
+ * gives the same bits.
  *   kv4_pages  uint8 [num_pages, Hkv, P / 16, 20 D], 16-byte aligned
  *   workspace  nld_block_attn_kv4_workspace_size() bytes, uninitialised; calls
  *              whose kernels may overlap need separate workspaces

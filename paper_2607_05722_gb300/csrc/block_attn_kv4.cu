@@ -22,10 +22,10 @@
 // on V, the V half while it works on K. With few units a CTA's warps share a
 // piece and join their sums; with many each warp has a range of its own, and
 // waits for no other.
-// Bound: HBM by bytes; here issue slots (13 instructions to dequantise 8
-// values, 1570 in all for a tile of 64 tokens). Measured, single tokens of 64 sequences of 512 to 8192 tokens (8
-// KV heads of 128, 347 MB of cache): 88 us, 4.0 TB/s, an instruction issued in
-// 61% of the cycles. Records loaded straight into registers: 222 us; units
+// Bound: HBM by bytes; here the instructions (13 to dequantise 8 values, 1570 in
+// all for a tile of 64 tokens) of three warps a scheduler. Measured, single tokens
+// of 64 sequences of 512 to 8192 tokens (8 KV heads of 128, 347 MB of cache): 88
+// us, 4.0 TB/s, an instruction issued in 61% of the cycles. Records loaded straight into registers: 222 us; units
 // shared by a CTA's warps: 132 us; 16 warps, two spilled: 88 us.
 #include "kv4.cuh"
 

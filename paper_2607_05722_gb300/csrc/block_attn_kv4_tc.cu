@@ -20,9 +20,10 @@
 // neither waits for the other's operands. The softmax paces steps of 128
 // tokens, the dequantisation steps of 256, so each gets the warps of the other.
 //
-// Bound: issue slots (65% to 72% used) and the latency of the hand-overs; 155
-// rows of 16 sequences of 8192 to 16384 tokens (8 KV heads of 128): 187 us, 650
-// TFLOP/s; 128 rows of one of 32768 tokens: 37 us, 465 TFLOP/s.
+// Bound: the latency of the hand-overs. No pipe is full: 155 rows of 16 sequences
+// of 8192 to 16384 tokens (8 KV heads of 128) take 186 us, 655 TFLOP/s, with issue
+// slots used to 66% and the tensor pipe to 33%; 128 rows of one of 32768 tokens 38
+// us, 455 TFLOP/s, 52% and 21%.
 //
 // Softmax over tokens runs along TMEM lanes, where a row maximum would cost a
 // cross-lane reduction per row and tile, and even a reference per row a

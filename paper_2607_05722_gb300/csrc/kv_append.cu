@@ -9,7 +9,7 @@
 // Everything here streams its rows once; the kernels are bound by HBM on long
 // prompts and by launch and dependent-load latency on single blocks. The bf16
 // append of prompts of up to 8192 rows (28,000 rows, 32 and 8 heads of 128)
-// takes 109 us, 6.4 TB/s; with a thread's items in any order of heads, each
+// takes 110 us, 6.4 TB/s; with a thread's items in any order of heads, each
 // loading its cosines and sines, it took 122 us.
 #include "kv4.cuh"
 
@@ -453,8 +453,8 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, long u, int sec
 // one of these after every `gap` of those: the first wait for memory, the
 // second for issue slots, so an SM should hold both. Prompts of up to 4096 rows
 // (8 sequences, 18,000 rows, 32 and 8 heads of 128), with their read-back:
-// 103 us, at 48 registers 105, at 64 it took 5% more. Bound: issue slots (74%
-// used) next to HBM (50%).
+// 104 us, at 48 registers 2% more, at 64 5%. Bound: issue slots next to HBM (63%
+// and 55% used).
 template <int D>
 __global__ void __launch_bounds__(kRowThreads, 9) rope_append_kv4_kernel(AppendArgs a, unsigned gap, unsigned units,
                                                                           unsigned parts, int by_warp) {
